@@ -191,9 +191,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
 
 def _ptr(x) -> Optional[int]:
     try:
-        return x.data_ptr()
-    except AttributeError:      # an address, or None
-        return x
+        return int(x.data_ptr())
+    except AttributeError:
+        if x is None or isinstance(x, int):     # an address
+            return x
+    # a host buffer among others, which ctypes would take for one
+    raise TypeError(f"a device buffer or an address expected, got {type(x).__name__}")
 
 
 def _stream(stream) -> Optional[int]:
