@@ -1016,6 +1016,7 @@ int make_plan_of(const cp_shape *s, const cp_sharing *sharing, Plan &pl)
     }
     double shared_us = 0.0;
     for (Part &part : pl.parts) {
+        if (part.tokens == 0) continue; // is not launched
         std::vector<int> shared_keys((size_t)part.requests, 0), ranges((size_t)part.requests, 0); // of every request
         std::vector<char> alone((size_t)part.requests, 0); // no item of own keys
         for (const Group &grp : part.groups) {
@@ -1030,7 +1031,7 @@ int make_plan_of(const cp_shape *s, const cp_sharing *sharing, Plan &pl)
                 own.add(E * G, s->h_prefix_lens[at] - shared_keys[(size_t)i] + E);
             }
         }
-        if (part.tokens > 0) choose_lengths(s, own, G, part);
+        choose_lengths(s, own, G, part);
         for (Group &grp : part.groups) {
             const int64_t n = (grp.keys + kBN - 1) / kBN, all = n + grp.new_tiles;
             const int64_t count = s->num_splits > 0 ? std::min<int64_t>({s->num_splits, n, kMaxRanges}) : group_ranges(grp, G, part.range_us);
