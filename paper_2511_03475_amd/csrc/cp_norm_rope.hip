@@ -109,13 +109,13 @@ __device__ __forceinline__ float inverse_rms(u32x4 raw, float eps, float &before
     const float mean = fmaf(sum, 1.f / kD, eps);
     before = 1.f;
     if (mean < 0x1p-100f) return __builtin_amdgcn_rsqf(mean * 0x1p100f) * 0x1p50f; // also where eps is no normal number
-    if (sum > 3.0e38f) {
+    if (fmaxf(sum, mean) > 3.0e38f) { // eps with the factor of the squares
         float x[8], small = 0.f;
         unpack(raw, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) small = fmaf(x[i] * 0x1p-70f, x[i] * 0x1p-70f, small);
         before = 0x1p-70f;
-        return __builtin_amdgcn_rsqf(head_sum(small) * (1.f / kD));
+        return __builtin_amdgcn_rsqf(fmaf(head_sum(small), 1.f / kD, eps * 0x1p-140f));
     }
     return __builtin_amdgcn_rsqf(mean);
 }
@@ -318,7 +318,7 @@ extern "C" int cp_qk_norm_rope(const void *q, const void *k, const void *v, cons
     if (rope->rotary_dim < 0 || rope->rotary_dim > kD || rope->rotary_dim % 16 != 0) return CP_ERR_SHAPE;
     if (rope->rotary_dim > 0 && !rope->h_inv_freq) return CP_ERR_NULL;
     if ((rope->interleaved | rope->weights_fp32) & ~1) return CP_ERR_SHAPE;
-    if (!(rope->eps > 0.f) || !(rope->eps < 3.0e38f) || !std::isfinite(rope->rotary_scale)) return CP_ERR_SHAPE;
+    if (!(rope->eps > 0.f) || !std::isfinite(rope->eps) || !std::isfinite(rope->rotary_scale)) return CP_ERR_SHAPE;
     const int Hq = shape->num_q_heads, Hkv = shape->num_kv_heads;
     const int heads[3] = {Hq, Hkv, Hkv};
     const int64_t strides[3] = {rope->q_stride, rope->k_stride, rope->v_stride};
