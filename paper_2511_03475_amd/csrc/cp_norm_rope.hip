@@ -96,7 +96,8 @@ __device__ __forceinline__ void unpack(const RopeParams &p, const void *from, We
 }
 
 // 1 / sqrt(mean of the squares + eps) of the 16 lanes' 8 elements each.  `before`: what the elements have to be multiplied by
-// first, 1 unless their squares leave the range of fp32, as those of finite bf16 values can.
+// first, 1 unless their squares or eps leave the range of fp32, as those of finite bf16 values can: above it, or where the
+// products below 2^-126, which the dot product takes for 0, make up more than 2^-29 of the mean.
 __device__ __forceinline__ float inverse_rms(u32x4 raw, float eps, float &before)
 {
     float sum = 0.f;
@@ -106,16 +107,15 @@ __device__ __forceinline__ float inverse_rms(u32x4 raw, float eps, float &before
         sum = __builtin_amdgcn_fdot2_f32_bf16(x, x, sum, false);
     }
     sum = head_sum(sum);
-    const float mean = fmaf(sum, 1.f / kD, eps);
-    before = 1.f;
-    if (mean < 0x1p-100f) return __builtin_amdgcn_rsqf(mean * 0x1p100f) * 0x1p50f; // also where eps is no normal number
-    if (fmaxf(sum, mean) > 3.0e38f) { // eps with the factor of the squares
-        float x[8], small = 0.f;
+    float mean = fmaf(sum, 1.f / kD, eps);
+    const bool high = fmaxf(sum, mean) > 3.0e38f;
+    before = high ? 0x1p-70f : mean < 0x1p-90f ? 0x1p60f : 1.f;
+    if (before != 1.f) {
+        float x[8], scaled = 0.f;
         unpack(raw, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) small = fmaf(x[i] * 0x1p-70f, x[i] * 0x1p-70f, small);
-        before = 0x1p-70f;
-        return __builtin_amdgcn_rsqf(fmaf(head_sum(small), 1.f / kD, eps * 0x1p-140f));
+        for (int i = 0; i < 8; ++i) scaled = fmaf(x[i] * before, x[i] * before, scaled);
+        mean = fmaf(head_sum(scaled), 1.f / kD, eps * before * before);
     }
     return __builtin_amdgcn_rsqf(mean);
 }
