@@ -883,42 +883,34 @@ void choose_lengths(const cp_shape *s, const OwnKeys &own, int G, Part &part)
             if (ranges > 1 || !grp.new_keys) part_rows += ranges * grp.tokens;
         }
         for (int b = 0; b < 2; ++b) batch[b].us /= (double)std::max<int64_t>(batch[b].count, 1);
-        // how many wavefronts share the own keys of a workgroup, each with no more blocks than a row tile's time has room for, or
-        // with 0.7 of that: the last to begin end earlier (48 requests with 16 new and up to 1500 tokens of their own 56 -> 50 us
-        // where the last cache has the keys, 60.6 -> 60.1 from memory; over all of the 600 batches it makes no difference)
+        // how many wavefronts share the own keys of a workgroup, each with no more blocks than a row tile's time has room for
         for (int waves = 1; waves <= kWaves && (waves == 1 || waves < 2 * most); waves *= 2) {
             const int64_t least = std::max<int64_t>(1, (most + kMaxRanges * waves - 1) / (kMaxRanges * waves));
-            const int64_t room = std::max(least, std::min((most + waves - 1) / waves, (int64_t)((item_us - kOwnStartUs) / kOwnBlockUs)));
-            int64_t before = 0;
-            for (const double of_room : {1.0, 0.7}) {
-                const int64_t each = std::max(least, (int64_t)((double)room * of_room));
-                if (each == before) continue;
-                before = each;
-                double items = 0.0, item_blocks = 0.0, parts_per_unit = 0.0, all_units = 0.0; // wavefronts, and blocks of each
-                for (int k = 0; k < 32; ++k) {
-                    if (own.units[k] == 0) continue;
-                    const double mean = (double)own.blocks[k] / (double)own.units[k], ranges = std::ceil(mean / (double)(each * waves));
-                    items += (double)own.units[k] * ranges * waves;
-                    item_blocks += (double)own.units[k] * ranges * waves * std::ceil(mean / ranges / waves);
-                    parts_per_unit += (double)own.units[k] * ranges;
-                    all_units += (double)own.units[k];
-                }
-                batch[2].count = (int64_t)std::ceil(items / kWaves) * heads;
-                batch[2].us = items > 0.0 ? kOwnStartUs + kOwnBlockUs * item_blocks / items : 0.0;
-                const double own_parts = items > 0.0 ? parts_per_unit / all_units * (double)own.tokens : 0.0;
-                const double join_us = (part_rows > 0 || own.tokens > 0 ? kJoinUs : 0.0) + 2.0 * (double)part_bytes(part_rows + (int64_t)own_parts, s->num_q_heads) / kPartBytesPerUs;
-                double work = 0.0;
-                for (const Batch &x : batch) work += (double)x.count * x.us;
-                if (best >= 0.0 && work / (double)cus + join_us >= best) continue;
-                const double longest_own = items > 0.0 ? kOwnStartUs + kOwnBlockUs * (double)each : 0.0;
-                // the longest may be the last to begin
-                const double us = std::max(makespan(batch, 3, cus) + 0.2 * std::max(0.0, longest_own - batch[2].us), longest_own) + join_us;
-                if (best < 0.0 || us < best) {
-                    best = us;
-                    part.range_us = range_us;
-                    part.own_waves = waves;
-                    part.own_blocks = (int)(each * waves);
-                }
+            const int64_t each = std::max(least, std::min((most + waves - 1) / waves, (int64_t)((item_us - kOwnStartUs) / kOwnBlockUs)));
+            double items = 0.0, item_blocks = 0.0, parts_per_unit = 0.0, all_units = 0.0; // wavefronts, and blocks of each
+            for (int k = 0; k < 32; ++k) {
+                if (own.units[k] == 0) continue;
+                const double mean = (double)own.blocks[k] / (double)own.units[k], ranges = std::ceil(mean / (double)(each * waves));
+                items += (double)own.units[k] * ranges * waves;
+                item_blocks += (double)own.units[k] * ranges * waves * std::ceil(mean / ranges / waves);
+                parts_per_unit += (double)own.units[k] * ranges;
+                all_units += (double)own.units[k];
+            }
+            batch[2].count = (int64_t)std::ceil(items / kWaves) * heads;
+            batch[2].us = items > 0.0 ? kOwnStartUs + kOwnBlockUs * item_blocks / items : 0.0;
+            const double own_parts = items > 0.0 ? parts_per_unit / all_units * (double)own.tokens : 0.0;
+            const double join_us = (part_rows > 0 || own.tokens > 0 ? kJoinUs : 0.0) + 2.0 * (double)part_bytes(part_rows + (int64_t)own_parts, s->num_q_heads) / kPartBytesPerUs;
+            double work = 0.0;
+            for (const Batch &x : batch) work += (double)x.count * x.us;
+            if (best >= 0.0 && work / (double)cus + join_us >= best) continue;
+            const double longest_own = items > 0.0 ? kOwnStartUs + kOwnBlockUs * (double)each : 0.0;
+            // the longest may be the last to begin
+            const double us = std::max(makespan(batch, 3, cus) + 0.2 * std::max(0.0, longest_own - batch[2].us), longest_own) + join_us;
+            if (best < 0.0 || us < best) {
+                best = us;
+                part.range_us = range_us;
+                part.own_waves = waves;
+                part.own_blocks = (int)(each * waves);
             }
         }
     }
