@@ -537,16 +537,24 @@ __device__ __forceinline__ bool find_request(const SharedParams &p, const Group 
         const int rr = base + lane;
         const int e = rr < p.batch ? p.extend_lens[rr] : 0;
         const int pl = rr < p.batch ? p.prefix_lens[rr] : 0;
-        int sl = 0, sr = 0, group = -1; // S and ranges of the lane's request
-        bool own = true;
-        for (int g = 0; g < p.groups; ++g) {
-            const int at_g = rr - __builtin_amdgcn_readlane(mine.request, g);
-            if (at_g >= 0 && at_g < __builtin_amdgcn_readlane(mine.requests, g)) {
-                sl = __builtin_amdgcn_readlane(mine.keys, g);
-                sr = __builtin_amdgcn_readlane(mine.ranges, g);
-                own = !__builtin_amdgcn_readlane(mine.new_keys, g);
-                group = g;
-            }
+        // The lane's group: groups lie one behind the other, so it is the last one that begins at the lane's request or in
+        // front of it, if it goes so far.  There is a bit for each of the 64 requests with which a group begins, and the bits up to
+        // the lane's are counted.  A look at every group, for every 64 requests, took longer than the keys: 32/8 heads, on 1024
+        // tokens and 40 of their own, 64 groups of 8 requests 222 us, 96 this way; 8 groups 18.6 and 17.8, one group the same.
+        const int begin = lane < p.groups ? mine.request - base : 64;
+        const uint32_t low = (uint32_t)__builtin_amdgcn_readlane(wave_scan(begin >= 0 && begin < 32 ? 1 << begin : 0), 63);
+        const uint32_t high = (uint32_t)__builtin_amdgcn_readlane(wave_scan(begin >= 32 && begin < 64 ? 1 << (begin - 32) : 0), 63);
+        const int before = __popcll(__builtin_amdgcn_ballot_w64(begin < 0));
+        const int here = (lane < 32 ? low >> lane : high >> (lane - 32)) & 1;
+        int group = before - 1 + here + (int)__builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0));
+        const int of = max(group, 0);
+        int sl = __shfl(mine.keys, of, 64), sr = __shfl(mine.ranges, of, 64); // S and ranges of the lane's request
+        bool own = !__shfl(mine.new_keys, of, 64);
+        const int end = __shfl(mine.request + mine.requests, of, 64);
+        if (group < 0 || rr >= end) {
+            sl = sr = 0;
+            group = -1;
+            own = true;
         }
         const int n = e > 0 && own ? own_ranges(pl - sl + e, p.own_blocks) : 0;
         const int parts = n + sr > 1 ? e * n : 0;
