@@ -27,21 +27,35 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E
 
 # HBM bytes per launch from two rocprofv3 --pmc runs (FETCH_SIZE x 2.0 + WRITE_SIZE x 1.0, scale
 # factors from a 1 GiB device copy in the same run), taken from the summaries under profiles/ and
-# valid only for the kernel source they were taken with: reported as null as soon as that source
-# changes.  They are not measured by this script.
+# valid only for the kernel source they were taken with, cp_extend.hip and the headers beside it that it includes:
+# reported as null as soon as one of them changes.  They are not measured by this script.
 TRAFFIC = {
-    "source_sha256_16": "420d3f372649d529",
+    "source_sha256_16": "23f0db98ea385bcf",
     "from": "profiles/extend_attn_kernel_long_context_32k.md, profiles/decode_attn_kernel_decode_b32_p10k.md",
-    "long_context_32k": (2130381 * 2.0 + 524301) * 1024.0,      # extend_attn_kernel
+    "long_context_32k": (2130378 * 2.0 + 524304) * 1024.0,      # extend_attn_kernel
     "decode_b32_p10k": (656295 * 2.0 + 256) * 1024.0,          # decode_attn_kernel
 }
 
 
-def measured_traffic(workload: str):
+def source_digest() -> str:
+    """Of cp_extend.hip and the files beside it that it includes, directly or through one another."""
     import hashlib
-    src = os.path.join(ROOT, "paper_2511_03475_amd", "csrc", "cp_extend.hip")
+    import re
+    folder = os.path.join(ROOT, "paper_2511_03475_amd", "csrc")
+    names = ["cp_extend.hip"]
+    digest = hashlib.sha256()
+    for name in names:      # grows while it is read
+        text = open(os.path.join(folder, name), "rb").read()
+        digest.update(text)
+        for other in re.findall(rb'^\s*#\s*include\s*"([^"]+)"', text, re.M):
+            if other.decode() not in names and os.path.exists(os.path.join(folder, other.decode())):
+                names.append(other.decode())
+    return digest.hexdigest()[:16]
+
+
+def measured_traffic(workload: str):
     try:
-        digest = hashlib.sha256(open(src, "rb").read()).hexdigest()[:16]
+        digest = source_digest()
     except OSError:
         return None
     if digest != TRAFFIC["source_sha256_16"]:
