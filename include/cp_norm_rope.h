@@ -16,7 +16,8 @@
  *     pair f: elements (f, f + rotary_dim / 2), or (2 f, 2 f + 1) if interleaved; elements behind
  *     rotary_dim stay as they are.
  * v is copied.  Sums and products are fp32, the result is rounded to bf16 once (nearest even).  The
- * angle is reduced in turns of 64-bit fixed point: it is exact to 2^-32 of a turn for every position.
+ * angle is reduced in turns of 64-bit fixed point, off by less than 2^-31 of a turn for every position, and then rounded to
+ * fp32, by at most 2^-26 of a turn.
  */
 #ifndef CP_NORM_ROPE_H
 #define CP_NORM_ROPE_H

@@ -35,7 +35,10 @@ typedef struct cp_sharing {
  * A new token's key or value that is not finite reaches rows of its own request alone.
  *
  * shape->num_splits: 0 lets the library choose, also whether the call runs with cp_extend_attention's own plan (groups
- * of one, short prefixes, or so many new tokens that reading is not what bounds the call); 1 .. 64 makes every group's
+ * of one, short prefixes, or so many new tokens that reading is not what bounds the call).  It chooses for the batch as a whole:
+ * requests with many new tokens that share nothing, a chunk of a prompt beside decoding, are best given to a call of their own
+ * (64 decoding requests on 32768 shared tokens 51 us, one chunk of 2048 tokens on 8192 by cp_extend_attention 278, both in one call
+ * 618; 32/8 heads).  1 .. 64 makes every group's
  * shared keys go over in that many ranges (fewer where it has fewer tiles of 64 keys), whatever the sizes.  The shared
  * plan scales scores in fp32: no query is rounded.
  *

@@ -6,14 +6,14 @@
 // Two kinds of range: of the group's S_g shared keys, which every row of the group sees whole, and of the request's
 // own keys, causal at the end.  One launch has both:
 //   row tiles   up to 256 rows of a (group, KV head), token by token, whatever request they are of, against a range of shared
-//               keys.  Eight wavefronts share tiles of 64 keys in LDS: each has 32 rows, or, of at most 128 rows, two have
-//               the same rows and take the tiles in turn
+//               keys.  Eight wavefronts share tiles of 64 keys in LDS: each has 32 rows, and those behind the last row only
+//               load
 //   own keys    32 rows of a (request, KV head) against a range of its own keys by one to eight wavefronts (cp_decode.h)
 // and a second one joins them.  Where no request of a group has cached tokens of its own, what is left are the new tokens, which
 // lie side by side: the row tiles of the last range go on over those of their requests, with a mask, and nothing is left
 // to join if there is one range.
 //
-// Measured, both launches: 64/8 heads, 128 requests with a new token on 131072 shared ones 517 us, bound by the matrix pipe (1.07
+// Measured, both launches: 64/8 heads, 128 requests with a new token on 131072 shared ones 522 us, bound by the matrix pipe (1.05
 // PFLOP/s; 3360 us request by request); 32/8 heads, 32 requests on 10240 24 us, bound by the chains start - tiles - join (12 us
 // of reading; 98 us); 48 in six groups with up to 1500 tokens of their own 60 us, 188 MB (183 us).
 #include <hip/hip_runtime.h>
@@ -792,7 +792,7 @@ size_t part_bytes(int64_t rows, int heads)
 // 128 rows and with fewer; own keys the same, a block of 32 keys.  Measured with 32/8 heads, one group, S = 10240: 32 tokens, all
 // keys in one range 1.03 a tile, in 27 ranges 1.24, 64 tokens 1.41; 64/8 heads, 128 tokens, S = 131072 2.0 (the clock falls
 // under that load); one tile of keys alone 6.9 with the launch, 20 blocks of own keys for each of 512 wavefronts 55.  The starts are
-// set a little longer than they are alone, for the plans that come of it: 600 drawn batches take 0.997 of the time with starts of 5.5 and 5.
+// set longer than they are alone, for the plans that come of it: 300 drawn batches take 0.99 of the time that 5.5 and 5 lead to.
 constexpr double kTileStartUs = 6.5, kTileUs = 1.75, kNarrowTileUs = 1.2, kOwnStartUs = 7.0, kOwnBlockUs = 2.6;
 constexpr double kLaunchUs = 0.4, kJoinUs = 4.0; // what comes on top of the first launch's work; the second with few partial results
 constexpr double kPartBytesPerUs = 5.0e6; // of partial results, written and read
@@ -930,8 +930,8 @@ void choose_lengths(const cp_shape *s, const OwnKeys &own, int G, Part &part)
 // 38 us, 32 96; 64/8 heads, 128 requests on 131072 3360; 100 requests on 20000 with 3000 of their own 766).  Where one
 // of the batch has more than kDecRows, they are read by fewer wavefronts, with two blocks of rows or next to row tiles: 61 requests
 // on 8615 tokens, 8/2 heads 134 us, 126 on 1344, 64/8 heads 132 (0.37 and 0.46 of it by the other rates).  The others are row
-// tiles, each over all keys.  Over 1000 drawn batches the plan that is taken has 1.009 of the time of the better one (1.018
-// with one pair of rates).
+// tiles, each over all keys.  Over 1000 drawn batches the plan that is taken has 1.006 of the time of the better one. One
+// plan is chosen for the whole batch.
 constexpr double kSplitKeys = 1024.0, kSplitUs = 4.0; // from so many keys on workgroups share them, and a merge comes behind
 constexpr double kOrdinaryStartUs = 6.7, kOwnBytesPerUs = 6.5e6, kSharedBytesPerUs = 1.5e7, kOwnTwoBytesPerUs = 5.0e6, kSharedTwoBytesPerUs = 7.5e6;
 double ordinary_us(const cp_shape *s, const cp_sharing *sharing, int G)
